@@ -76,6 +76,19 @@ __device__ __forceinline__ f32x4 unpack_half4(u32x2 p) {
     return v;
 }
 
+// What a number is multiplied by for a division by a norm: a power of two, then the rest.  In one fp32 number the reciprocal of a norm below
+// 2^-128 (momentum that no gradient has reached for long ends there) would be an infinity, of one beyond 2^126 it would lose digits.
+struct Divisor {
+    float power, rest;
+};
+__device__ __forceinline__ Divisor divisor(double norm) {
+    if (norm == 0.) return {1.f, 0.f};
+    // (an infinity, whose exponent is taken as 0, brings finite numbers to 0 and itself, as NaN does everything, to NaN)
+    const int e = -__builtin_amdgcn_frexp_exp(norm), power = max(-126, min(126, e));
+    return {__builtin_ldexpf(1.f, power), (float)__builtin_ldexp(1. / __builtin_amdgcn_frexp_mant(norm), e - power)};
+}
+__device__ __forceinline__ float divide(float u, Divisor by) { return u * by.power * by.rest; }
+
 // work-groups of the passes over a matrix: at least 16 elements a thread; of the first one also sums of squares
 __host__ __device__ inline int norm_blocks(const Mat& q) {
     const long b = ((long)q.rows * q.cols + 4095) / 4096;
@@ -160,8 +173,7 @@ __global__ __launch_bounds__(256) void ns_scale_kernel(const Group g, const Rule
     for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
     if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = sum;
     __syncthreads();
-    const double norm = sqrt(sums[0] + sums[1] + sums[2] + sums[3]) + (double)r.eps;
-    const float inv = norm == 0. ? 0.f : (float)(1. / norm);
+    const Divisor by = divisor(sqrt(sums[0] + sums[1] + sums[2] + sums[3]) + (double)r.eps);
     const bool vec = q.cols % 4 == 0;
     for (unsigned i = block * 256 + threadIdx.x; i < groups; i += blocks * 256) {
         const unsigned row = i / per;
@@ -184,7 +196,7 @@ __global__ __launch_bounds__(256) void ns_scale_kernel(const Group g, const Rule
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             if (r.muon) u[e] = r.nesterov ? __builtin_fmaf(r.momentum, mv[e], u[e]) : mv[e];
-            u[e] *= inv;
+            u[e] = divide(u[e], by);
         }
         store_x(u, reinterpret_cast<u32x2*>(q.x16) + i, reinterpret_cast<u32x2*>(q.low16) + i);
     }
@@ -475,9 +487,9 @@ struct SmallX {
 };
 __device__ __forceinline__ u32x2 half4(f32x4 v) { return pack_half4(f32x4{v[0] * kScaleX, v[1] * kScaleX, v[2] * kScaleX, v[3] * kScaleX}); }
 
-// Sums of X X^T over the wavefront's columns (times `by` squared), tiles (i, j) with j <= i, into the LDS.
+// Sums of X X^T over the wavefront's columns, tiles (i, j) with j <= i, into the LDS.
 template <int BLOCKS>
-__device__ __forceinline__ void small_gram(const SmallX<BLOCKS>& s, float by, unsigned char* smem, int wave, int lane) {
+__device__ __forceinline__ void small_gram(const SmallX<BLOCKS>& s, unsigned char* smem, int wave, int lane) {
     const int l16 = lane & 15, l4 = lane >> 4;
     unsigned char* strip = smem + wave * kSmallTiles * 1024;
     static_assert(kSmallStrip <= kSmallTiles * 1024, "a strip fits the wavefront's sums");
@@ -492,10 +504,7 @@ __device__ __forceinline__ void small_gram(const SmallX<BLOCKS>& s, float by, un
 #pragma unroll
             for (int i = 0; i < 4; ++i) {  // [column][row]
                 u32x2 v = {0u, 0u};
-                if (b + h < BLOCKS) {
-                    const f32x4 f = s.x[b + h < BLOCKS ? b + h : b][i];
-                    v = half4(f32x4{f[0] * by, f[1] * by, f[2] * by, f[3] * by});
-                }
+                if (b + h < BLOCKS) v = half4(s.x[b + h < BLOCKS ? b + h : b][i]);
                 *reinterpret_cast<u32x2*>(strip + (h * 16 + l16) * 144 + (i * 16 + l4 * 4) * 2) = v;
             }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -692,7 +701,15 @@ __device__ __forceinline__ double small_squares(const SmallX<BLOCKS>& s, double*
     for (int w = 0; w < kSmallWaves; ++w) square += meet[w];
     return square;
 }
-__device__ __forceinline__ float inverse(double norm) { return norm == 0. ? 0.f : (float)(1. / norm); }
+template <int BLOCKS>
+__device__ __forceinline__ void small_divide(SmallX<BLOCKS>& s, Divisor by) {
+#pragma unroll
+    for (int b = 0; b < BLOCKS; ++b)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s.x[b][i][e] = divide(s.x[b][i][e], by);
+}
 
 // All of a matrix in one work-group: X in the registers, A and B in the LDS, every step behind the other without a launch.  Bound by its
 // chain of dependent products and barriers: 64 x 576 with five steps 34 us (in 17 launches: 69).
@@ -703,15 +720,9 @@ __global__ __launch_bounds__(kSmallThreads, 2) void ns_small_kernel(const Group 
     const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), n = min(q.rows, q.cols);
     SmallX<BLOCKS> s;
     small_read(s, q, r, 0, wave, lane);
-    const float inv = inverse(sqrt(small_squares(s, reinterpret_cast<double*>(smem + kSmallLds - 256), wave, lane)) + (double)r.eps);
-#pragma unroll
-    for (int b = 0; b < BLOCKS; ++b)
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) s.x[b][i][e] *= inv;
+    small_divide(s, divisor(sqrt(small_squares(s, reinterpret_cast<double*>(smem + kSmallLds - 256), wave, lane)) + (double)r.eps));
     for (int k = 0; k < steps; ++k) {
-        small_gram(s, 1.f, smem, wave, lane);
+        small_gram(s, smem, wave, lane);
         small_step(s, r, n, smem, t, [&](int at) { return small_sum(smem, at); });
     }
     small_write(s, q, r, 0, wave, lane);
@@ -728,11 +739,10 @@ __global__ __launch_bounds__(kSmallThreads, 2) void ns_many_kernel(const Group g
     f32x4* x32 = reinterpret_cast<f32x4*>(q.x32) + (size_t)block * kManyBlocks * 4 * kSmallThreads + t;
     f32x4* sums = reinterpret_cast<f32x4*>(q.sums) + (step & 1) * blocks * kSmallQuads;  // of this step; the other half: the next one's
     SmallX<kManyBlocks> s;
-    float by = 1.f;
+    double square = 0.;
     if (step == 0) {
         small_read(s, q, r, c0, wave, lane);
-        const double square = small_squares(s, meet, wave, lane);
-        by = inverse(sqrt(square));
+        square = small_squares(s, meet, wave, lane);
         if (t == 0) q.parts[block] = square;
     } else {
 #pragma unroll
@@ -740,17 +750,10 @@ __global__ __launch_bounds__(kSmallThreads, 2) void ns_many_kernel(const Group g
 #pragma unroll
             for (int i = 0; i < 4; ++i) s.x[b][i] = x32[(b * 4 + i) * kSmallThreads];
         if (step == 1) {
-            double square = 0.;
             for (int p = 0; p < blocks; ++p) square += q.parts[p];
             const double norm = sqrt(square) + (double)r.eps;
-            const float inv = inverse(norm);
-#pragma unroll
-            for (int b = 0; b < kManyBlocks; ++b)
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) s.x[b][i][e] *= inv;
-            // (a share of the columns without any entry has no norm and no sums)
+            small_divide(s, divisor(norm));
+            // (a share of the columns without any entry has no norm and no sums; one next to nothing has finite sums and a share of 0)
             small_step(s, r, n, smem, t, [&](int k) {
                 f32x4 v = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 8
@@ -783,7 +786,8 @@ __global__ __launch_bounds__(kSmallThreads, 2) void ns_many_kernel(const Group g
     for (int b = 0; b < kManyBlocks; ++b)
 #pragma unroll
         for (int i = 0; i < 4; ++i) x32[(b * 4 + i) * kSmallThreads] = s.x[b][i];
-    small_gram(s, by, smem, wave, lane);
+    if (step == 0) small_divide(s, divisor(sqrt(square)));
+    small_gram(s, smem, wave, lane);
     f32x4* next = reinterpret_cast<f32x4*>(q.sums) + ((step + 1) & 1) * blocks * kSmallQuads + (size_t)block * kSmallQuads;
     for (int k = t; k < kSmallQuads; k += kSmallThreads) next[k] = small_sum(smem, k);
 }
