@@ -5,8 +5,9 @@
 //
 // Precision: products on fp16 operands (11 significant bits at bf16's rate; everything here is bounded: |X| by its largest singular value,
 // which starts at 1 or less) scaled by powers of two away from fp16's subnormals, sums in fp32.  X itself is kept with 22 bits for the term
-// a X, as that operand and what its rounding left, in fp16 too (fp32 beside the operand is two bytes an element more each way): small singular values live in that term alone, and an X rounded from step to step would drown them in the rounding of
-// the large ones.  Where the singular values are close to each other, B is near a multiple of the identity that cancels most of a; that
+// a X, as that operand and what its rounding left, in fp16 too (fp32 beside the operand is two bytes an element more each way) and times 2^11,
+// or what is left of elements below 2^-13 would be among fp16's subnormals; below 2^-24, where the operand is, X is kept to 2^-46.
+// Small singular values live in that term alone, and an X rounded from step to step would drown them in the rounding of the large ones.  Where the singular values are close to each other, B is near a multiple of the identity that cancels most of a; that
 // multiple, b t + c t t with t the mean of A's diagonal, then goes to the term in fp32 too: X <- (a + shift) X + (B - shift) X.
 // (t^2 n > 0.8 |A|^2 says so.  With small singular values among large ones the shifted products would bring the roundings back.)
 // Simulated error of the result, 512 x 768 of rank 8: 0.34 with bf16 throughout, 0.04 with fp16, 3e-4 so; full-rank
@@ -26,7 +27,7 @@ typedef __attribute__((ext_vector_type(2))) float f32x2;
 
 constexpr int kMaxGroup = 16;  // matrices of one set of launches
 // what is stored as fp16 times a power of two: X, A = X X^T, B
-constexpr float kScaleX = 0x1p10f, kScaleA = 0x1p12f, kScaleB = 0x1p10f;
+constexpr float kScaleX = 0x1p10f, kScaleA = 0x1p12f, kScaleB = 0x1p10f, kScaleLow = 0x1p11f;  // (Low: of what X's operand left, once more)
 
 struct Mat {
     int rows, cols, pitch;  // pitch: columns rounded up to 8, zeros behind the last
@@ -158,7 +159,7 @@ __device__ __forceinline__ void store_x(f32x4 x, u32x2* high, u32x2* low) {
     const u32x2 h = pack_half4(y);
     const f32x4 back = unpack_half4(h);
     *high = h;
-    *low = pack_half4(f32x4{y[0] - back[0], y[1] - back[1], y[2] - back[2], y[3] - back[3]});
+    *low = pack_half4(f32x4{(y[0] - back[0]) * kScaleLow, (y[1] - back[1]) * kScaleLow, (y[2] - back[2]) * kScaleLow, (y[3] - back[3]) * kScaleLow});
 }
 
 // X of the first step, in rows of whole groups of eight with zeros behind.  (U is computed again rather than stored by the pass before, which
@@ -434,7 +435,7 @@ __global__ __launch_bounds__(W::THREADS, W::THREADS >= 512 ? 2 : 1) void ns_appl
         const size_t at = (size_t)n * q.pitch + m;
         const f32x4 high = unpack_half4(x.high), low = unpack_half4(x.low);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = __builtin_fmaf(ra * (1.f / kScaleX), high[e] + low[e], v[e] * (1.f / (kScaleX * kScaleB)));
+        for (int e = 0; e < 4; ++e) v[e] = __builtin_fmaf(ra * (1.f / kScaleX), __builtin_fmaf(low[e], 1.f / kScaleLow, high[e]), v[e] * (1.f / (kScaleX * kScaleB)));
         if (!r.last) {
             store_x(v, reinterpret_cast<u32x2*>(q.next16 + at), reinterpret_cast<u32x2*>(q.low16 + at));
             return;
