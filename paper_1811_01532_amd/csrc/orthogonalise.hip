@@ -50,8 +50,10 @@ struct Mat {
     int split;       // parts of the reduction of X X^T
     float* part;     // ... their sums: [tile][part][64][64]
 };
+enum Way { ONE, MANY, TILES };  // a work-group a matrix and one launch; several of them and a launch a step; products on tiles
 struct Group {
     int n, blocks;
+    Way way;
     int gram, square, apply;  // tiles of the three products
     bool split;               // X X^T in parts (small tiles)
     Mat mat[kMaxGroup];
@@ -840,8 +842,18 @@ int squares(const Mat& q, int tile) {
 }
 int whole(const Mat& q, int tile) { return tiles_across(q.rows, tile) * tiles_across(q.cols, tile); }
 
-// How a group's products run.
+// How a group runs.
 void plan(Group& g) {
+    // Matrices of few rows take one launch, or one a step; beside a larger one they ride along in its launches for nothing.
+    int columns = 0, groups = 0;
+    bool few = true;
+    for (int i = 0; i < g.n; ++i) {
+        few = few && g.mat[i].n <= kSmallRows;
+        columns = std::max(columns, std::max(g.mat[i].rows, g.mat[i].cols));
+        groups = std::max(groups, many_blocks(g.mat[i]));
+    }
+    g.way = few && columns <= kSmallBlocks[1] * 16 * kSmallWaves ? ONE : few && groups <= kManyMost ? MANY : TILES;
+    if (g.way != TILES) return;
     // Which tile: the work on the fullest CU (X X^T at 512 x 4608 takes 99 / 41 / 18 us on tiles of 256 / 128 / 64, at 2048 x 2048
     // 55 / 26 / 24, at 4096 x 4096 102 / 120 / 149).
     auto pick = [&](auto&& tiles, auto&& depth, bool store, double* us_out) {
@@ -895,27 +907,30 @@ void plan(Group& g) {
 }
 
 size_t up256(size_t b) { return (b + 255) & ~(size_t)255; }
-// Lays a matrix's scratch out behind `at`; base == NULL: only its size.
-size_t place(Mat& q, bool split, unsigned char* base, size_t at) {
+// Lays a matrix's scratch out behind `at`, as far as its group's way needs it (one work-group: nothing lies in memory); base == NULL: only its size.
+size_t place(Mat& q, const Group& g, unsigned char* base, size_t at) {
     auto take = [&](size_t bytes) {
         unsigned char* p = base ? base + at : nullptr;
         at += up256(bytes);
         return p;
     };
-    const size_t elems = (size_t)q.rows * q.pitch, square = (size_t)q.n * q.npitch;
-    const size_t many = q.n <= kSmallRows ? (size_t)many_blocks(q) : 0;
     q.parts = (double*)take(256 * sizeof(double));
-    q.shift = (float*)take(4);
-    const size_t tiles = (size_t)(q.n + 63) / 64;
-    q.moments = (f32x2*)take(tiles * (tiles + 1) / 2 * sizeof(f32x2));
-    q.x32 = (float*)take(many * kManyBlocks * kSmallThreads * 4 * sizeof(f32x4));
-    q.low16 = (bf16_t*)take(elems * 2);
-    q.sums = (float*)take(2 * many * kSmallQuads * sizeof(f32x4));
-    q.x16 = (bf16_t*)take(elems * 2);
-    q.next16 = (bf16_t*)take(elems * 2);
-    q.a16 = (bf16_t*)take(square * 2);
-    q.b16 = (bf16_t*)take(square * 2);
-    if (split) q.part = (float*)take((size_t)squares(q, 64) * q.split * 4096 * sizeof(float));
+    if (g.way == MANY) {
+        const size_t groups = (size_t)many_blocks(q);
+        q.x32 = (float*)take(groups * kManyBlocks * kSmallThreads * 4 * sizeof(f32x4));
+        q.sums = (float*)take(2 * groups * kSmallQuads * sizeof(f32x4));
+    }
+    if (g.way == TILES) {
+        const size_t elems = (size_t)q.rows * q.pitch, square = (size_t)q.n * q.npitch, tiles = (size_t)(q.n + 63) / 64;
+        q.shift = (float*)take(4);
+        q.moments = (f32x2*)take(tiles * (tiles + 1) / 2 * sizeof(f32x2));
+        q.low16 = (bf16_t*)take(elems * 2);
+        q.x16 = (bf16_t*)take(elems * 2);
+        q.next16 = (bf16_t*)take(elems * 2);
+        q.a16 = (bf16_t*)take(square * 2);
+        q.b16 = (bf16_t*)take(square * 2);
+        if (g.split) q.part = (float*)take((size_t)squares(q, 64) * q.split * 4096 * sizeof(float));
+    }
     return at;
 }
 
@@ -964,17 +979,12 @@ int launch_part(const Group& g, hipStream_t st) {
 
 int run_group(Group& g, Rule r, int steps, hipStream_t st) {
     int rc;
-    // Matrices of few rows take one launch, or one a step; beside a larger one they ride along in its launches for nothing.
-    int most = 0, most_many = 0;
-    bool small = true;
-    for (int i = 0; i < g.n; ++i) {
-        small = small && g.mat[i].n <= kSmallRows;
-        most = std::max(most, tiles_across(std::max(g.mat[i].rows, g.mat[i].cols), 16 * kSmallWaves));
-        most_many = std::max(most_many, many_blocks(g.mat[i]));
-    }
-    if (small && most <= kSmallBlocks[1])
+    if (g.way == ONE) {
+        int most = 0;
+        for (int i = 0; i < g.n; ++i) most = std::max(most, tiles_across(std::max(g.mat[i].rows, g.mat[i].cols), 16 * kSmallWaves));
         return most <= kSmallBlocks[0] ? launch_small<kSmallBlocks[0]>(g, r, steps, st) : launch_small<kSmallBlocks[1]>(g, r, steps, st);
-    if (small && most_many <= kManyMost) {
+    }
+    if (g.way == MANY) {
         static std::atomic<bool> allowed{false};
         if (!allowed) {
             const hipError_t e = hipFuncSetAttribute((const void*)ns_many_kernel, hipFuncAttributeMaxDynamicSharedMemorySize, kSmallLds);
@@ -1036,7 +1046,7 @@ Group next_group(int n, int* i, unsigned char* base, size_t* bytes, F&& at) {
     }
     plan(g);
     *bytes = 0;
-    for (int k = 0; k < g.n; ++k) *bytes = place(g.mat[k], g.split, base, *bytes);
+    for (int k = 0; k < g.n; ++k) *bytes = place(g.mat[k], g, base, *bytes);
     return g;
 }
 template <class F>
