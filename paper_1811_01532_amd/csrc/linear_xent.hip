@@ -815,8 +815,8 @@ Layout layout(const wap_linear_xent_desc& d, bool grads) {
     l.parts = take(N * (size_t)l.nparts * sizeof(Part));
     if (l.keep || l.logits.parts > 1) l.z = take(zbytes * l.logits.parts);
     if (grads) {
-        // pieces of equal size whose gradient of the logits stays in the chip's cache
-        const int most = l.few ? all : (int)std::max<size_t>(8, kPieceBytes / (512 * N));
+        // pieces of equal size whose gradient of the logits stays in the chip's cache, and its rows within what a tile can address
+        const int most = l.few ? all : (int)std::min<size_t>(kMaxPitch / 256, std::max<size_t>(8, kPieceBytes / (512 * N)));
         l.npieces = (all + most - 1) / most;
         const int per = (all + l.npieces - 1) / l.npieces;
         l.piece = per * 256;
