@@ -730,7 +730,10 @@ int launch_grad(int tile, const GradArgs& a, int parts, hipStream_t st) {
 }
 template <bool N_IROWS>
 int launch_grad(int tile, const GradArgs& a, int parts, hipStream_t st) {
-    return a.a.end ? launch_grad<N_IROWS, true>(tile, a, parts, st) : launch_grad<N_IROWS, false>(tile, a, parts, st);
+    if constexpr (!N_IROWS) {  // (dx: the weights may be ragged; rows of x that dW takes have been gathered)
+        if (a.a.end) return launch_grad<N_IROWS, true>(tile, a, parts, st);
+    }
+    return launch_grad<N_IROWS, false>(tile, a, parts, st);
 }
 
 int launch_pad(const bf16_t* src, long pitch, int rows, int len, int to, bf16_t* dst, hipStream_t st) {
