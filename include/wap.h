@@ -243,8 +243,8 @@ int wap_sgd_update(int64_t n, float* w32, const float* dw, float lr, void* w_bf1
 /* Newton-Schulz iteration of a matrix U:  X = U / (|U| + eps), |.| the Frobenius norm (X = 0 where that sum is 0);
  * `steps` times:  A = X X^T,  X <- a X + (b A + c A A) X   (X^T X from the right for more rows than columns),
  * which takes every singular value s of X to a s + b s^3 + c s^5 and keeps the singular vectors.
- * Products take fp16 operands and sum in fp32; X is kept to 22 bits of each element, and no finer than 2^-46, from step to step.  Coefficients that let singular values grow beyond
- * about 4 leave the range of the operands and give infinities or NaN. */
+ * Products take fp16 operands and sum in fp32; X is kept to 22 bits of each element, and no finer than 2^-46, from step to step.
+ * Coefficients that let singular values grow beyond about 4 leave the range of the operands and give infinities or NaN. */
 typedef struct {
     float a, b, c, eps;
     int32_t steps; /* 1 .. 100 */

@@ -7,7 +7,8 @@
 // which starts at 1 or less) scaled by powers of two away from fp16's subnormals, sums in fp32.  X itself is kept with 22 bits for the term
 // a X, as that operand and what its rounding left, in fp16 too (fp32 beside the operand is two bytes an element more each way) and times 2^11,
 // or what is left of elements below 2^-13 would be among fp16's subnormals; below 2^-24, where the operand is, X is kept to 2^-46.
-// Small singular values live in that term alone, and an X rounded from step to step would drown them in the rounding of the large ones.  Where the singular values are close to each other, B is near a multiple of the identity that cancels most of a; that
+// Small singular values live in that term alone, and an X rounded from step to step would drown them in the rounding of the large ones.
+// Where the singular values are close to each other, B is near a multiple of the identity that cancels most of a; that
 // multiple, b t + c t t with t the mean of A's diagonal, then goes to the term in fp32 too: X <- (a + shift) X + (B - shift) X.
 // (t^2 n > 0.8 |A|^2 says so.  With small singular values among large ones the shifted products would bring the roundings back.)
 // Simulated error of the result, 512 x 768 of rank 8: 0.34 with bf16 throughout, 0.04 with fp16, 3e-4 so; full-rank
@@ -714,8 +715,9 @@ __device__ __forceinline__ void small_divide(SmallX<BLOCKS>& s, Divisor by) {
             for (int e = 0; e < 4; ++e) s.x[b][i][e] = divide(s.x[b][i][e], by);
 }
 
-// All of a matrix in one work-group: X in the registers, A and B in the LDS, every step behind the other without a launch.  Bound by its
-// chain of dependent products and barriers: 64 x 576 with five steps 34 us (in 17 launches: 69).
+// All of a matrix in one work-group: X in the registers, A and B in the LDS, every step behind the other without a launch.  64 x 576 with
+// five steps takes 34 us (in 17 launches: 69): 4.5 a step, bound by its chain of sums through the LDS, dependent products and barriers,
+// and 11 for the launch, the loads (a block of columns waits for the one before), the norm and the stores.
 template <int BLOCKS>
 __global__ __launch_bounds__(kSmallThreads, 2) void ns_small_kernel(const Group g, const Rule r, int steps) {
     extern __shared__ __align__(16) unsigned char smem[];
